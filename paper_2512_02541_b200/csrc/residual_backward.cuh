@@ -1,9 +1,10 @@
 // The residual stream, backward; residual.cuh has what both directions share.
 //
-// With x the centred r, g = dh * A (A the norm's weight) and rho the reciprocal deviation:
-//   d = dr + rho * (g - mean(g)) - x * rho^3 * mean(g x),     dx = alpha * d          (mean(g) with a mean in the norm only)
+// With xhat the standardised r, g = dh * A (A the norm's weight) and rho the reciprocal deviation:
+//   d = dr + rho * (g - mean(g) - xhat * mean(g xhat)),     dx = alpha * d            (mean(g) with a mean in the norm only)
 // With yhat the standardised y, e = gate * post_weight * d:   dy = rho_y * (e - mean(e) - yhat * mean(e yhat)); without a post norm
-// dy = gate * d.  Sums over tokens, per channel:
+// dy = gate * d.  Rows are standardised before they are multiplied by anything: rho^2 and rho^3 leave the range of 32 bits long before rho
+// does (rows beyond 1e12, and rows of zeros, which fill up a short batch, behind an eps below 2e-26).  Sums over tokens, per channel:
 //   A: dh * xhat -> dweight        B: dh -> dbias
 //   S: d * yhat (d * y without a post norm)       N: d             (N only behind a post norm)
 //   dgate = post_weight * S + post_bias * N,  dpost_weight = gate * S,  dpost_bias = gate * N      (dgate = S without a post norm)
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
     const auto get_dh = [&](int j, float (&v)[RUNS][kRun]) { get(dhq, j, 2 * rb, v); };
     const auto get_y = [&](int j, float (&v)[RUNS][kRun]) { get(yq, j, 2 * rb + bb, v); };
 
-    float mean[R], y_m[R], rstd[R], y_rstd[R], pull[R], shift[R];
+    float mean[R], y_m[R], rstd[R], y_rstd[R], pull[R], shift[R];          // pull, shift: -mean(g xhat) and -mean(g)
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       mean[j] = next_mean[j];
@@ -329,8 +330,8 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
       if (!POST && early) next_mean[j] = more[4 * j + 3] * a.inv_c;
       if (POST) y_rstd[j] = rsqrtf(more[4 * j + 3] * a.inv_c + a.post_eps);
       rstd[j] = rsqrtf(more[4 * j] * a.inv_c + a.eps);
-      if (r_mean) shift[j] = -rstd[j] * (more[4 * j + 1] * a.inv_c);
-      pull[j] = -rstd[j] * rstd[j] * rstd[j] * (more[4 * j + 2] * a.inv_c);
+      if (r_mean) shift[j] = -more[4 * j + 1] * a.inv_c;
+      pull[j] = -rstd[j] * (more[4 * j + 2] * a.inv_c);
     }
     float dots[LAY > 2 ? 4 * R : 2 * R], e[POST ? R : 1][RUNS][kRun];
 #pragma unroll
@@ -347,9 +348,9 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
         for (int i = 0; i < RUNS; ++i)
 #pragma unroll
           for (int k = 0; k < kRun; k += 2) {
-            const uint64_t xx = two(x[i] + k), tt = mul_f32x2(two(t[i] + k), rr);
-            put_two(fma_f32x2(tt, xx, two(sA[i] + k)), sA[i] + k);
-            put_two(add_f32x2(fma_f32x2(tt, two(A[i] + k), two(d[i] + k)), fma_f32x2(xx, pp, ss)), d[i] + k);
+            const uint64_t xhat = mul_f32x2(two(x[i] + k), rr), tt = two(t[i] + k);
+            put_two(fma_f32x2(tt, xhat, two(sA[i] + k)), sA[i] + k);
+            put_two(fma_f32x2(fma_f32x2(xhat, pp, fma_f32x2(tt, two(A[i] + k), ss)), rr, two(d[i] + k)), d[i] + k);
           }
       }
       if (a.dx && j < n) {
@@ -408,8 +409,7 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         if (!a.dy || j >= n) continue;
-        // rho (e - mean(e)) - y rho^2 mean(e yhat), with y centred
-        const float back = y_mean ? -y_rstd[j] * (dots[2 * j] * a.inv_c) : 0.f, dot = -y_rstd[j] * y_rstd[j] * (dots[2 * j + 1] * a.inv_c);
+        const float back = y_mean ? -dots[2 * j] * a.inv_c : 0.f, dot = -dots[2 * j + 1] * a.inv_c;      // -mean(e), -mean(e yhat)
         const uint64_t mm = pack_f32x2(back, back), qq = pack_f32x2(dot, dot), rr = pack_f32x2(y_rstd[j], y_rstd[j]);
         float yv[RUNS][kRun];
         get_y(j, yv);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
         for (int i = 0; i < RUNS; ++i) {
 #pragma unroll
           for (int k = 0; k < kRun; k += 2)
-            put_two(fma_f32x2(two(e[j][i] + k), rr, fma_f32x2(two(yv[i] + k), qq, mm)), e[j][i] + k);
+            put_two(mul_f32x2(fma_f32x2(mul_f32x2(two(yv[i] + k), rr), qq, add_f32x2(two(e[j][i] + k), mm)), rr), e[j][i] + k);
           ch.template write<TB>(e[j][i], dy, i);
         }
         dy += a.dys;
