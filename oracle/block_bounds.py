@@ -88,6 +88,23 @@ def residual_backward(op, dh, dr, r, y, weight=None, bias=None, gate=None, post_
     return bounds
 
 
+def rotary_backward(op, dout, x, positions, weight=None):
+    """-> what dx, dweight and dbias of ``op`` (block_oracle.Rotary) may be off by; dx in front of its rounding.  A cosine or sine is off by
+    fewer than 4 U: the last bit of an angle in half turns (pi 2^-25) and the function's own two."""
+    dout = np.asarray(dout, np.float64)
+    size = np.abs(dout)
+    for a, b, _, _ in op.layout():
+        size[..., a] = size[..., b] = np.abs(dout[..., a]) + np.abs(dout[..., b])
+    e, e_err = op.turn(dout, positions, back=True), 8 * U * size
+    if op.norm == orc.NONE:
+        return e_err, None, None
+    st = Standard(x, op.norm, op.eps)
+    w = 1.0 if weight is None else np.asarray(weight, np.float64)
+    summed = lambda terms, errors: errors.sum((0, 1)) + CHAIN * U * np.abs(terms).sum((0, 1))
+    dx = st.back(e * w, e_err * np.abs(w) + U * np.abs(e * w))
+    return dx, summed(e * st.xhat, e_err * np.abs(st.xhat) + np.abs(e) * st.err), summed(e, e_err)
+
+
 def half_step(want, step, smallest):
     """What rounding to a type of that step (eps) and smallest value may move a value by."""
     return step / 2 * np.abs(want) * (1 + 2.0 ** -8) + smallest

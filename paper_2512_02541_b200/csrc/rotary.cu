@@ -503,7 +503,8 @@ __global__ void __launch_bounds__(32 * kWarps, kBlocksPerSm) rotary_kernel(const
 }
 
 // Backward behind a norm.  With e = the gradient turned back, xhat the standardised head and g = e * weight:
-//   dx = rstd * (g - mean(g) - xhat * mean(g * xhat))      (mean(g) with a mean in the norm only)
+//   dx = rstd * (g - mean(g) - xhat * mean(g * xhat))      (mean(g) with a mean in the norm only; xhat is formed
+//                                                           first: rstd^3 leaves the range of 32 bits long before rstd does)
 //   dweight = sum of e * xhat, dbias = sum of e            over tokens and heads
 // The sums are kept by the lane that holds the elements, over all the tokens of its warp; a thread block works on one tensor, so that a
 // lane has one tensor's sums to keep.  The blocks' sums go to the workspace and are added up by rotary_sums_kernel.  With 64 registers of
@@ -631,16 +632,16 @@ __global__ void __launch_bounds__(32 * kWarps, kBackBlocksPerSm) rotary_backward
       sum = head_sum<LANES>(sum, a.lanes);
       dot = head_sum<LANES>(dot, a.lanes);
       const float rstd = rsqrtf(sq * a.inv_d + a.eps);
-      // with x centred: rstd * g - rstd * mean(g) - x * (rstd^3 * mean(g x))
-      const float shift = a.norm == AVGGT_NORM_LAYER ? -rstd * sum * a.inv_d : 0.f, pull = -rstd * rstd * rstd * (dot * a.inv_d);
+      // -rstd * mean(g) and, of xhat, -rstd * mean(g xhat)
+      const float shift = a.norm == AVGGT_NORM_LAYER ? -rstd * (sum * a.inv_d) : 0.f, pull = -rstd * (rstd * (dot * a.inv_d));
       const uint64_t rr = pack_f32x2(rstd, rstd), pp = pack_f32x2(pull, pull), sh = pack_f32x2(shift, shift);
 #pragma unroll
       for (int i = 0; i < NU; ++i)
 #pragma unroll
         for (int e = 0; e < 2 * PU; e += 2) {
-          const uint64_t xx = two(x[i] + e);
-          put_two(fma_f32x2(two(g[i] + e), mul_f32x2(xx, rr), two(dw[i] + e)), dw[i] + e);
-          put_two(fma_f32x2(two(gw[i] + e), rr, fma_f32x2(xx, pp, sh)), gw[i] + e);
+          const uint64_t xhat = mul_f32x2(two(x[i] + e), rr);
+          put_two(fma_f32x2(two(g[i] + e), xhat, two(dw[i] + e)), dw[i] + e);
+          put_two(fma_f32x2(two(gw[i] + e), rr, fma_f32x2(xhat, pp, sh)), gw[i] + e);
         }
       grad.set(gw);
     }
