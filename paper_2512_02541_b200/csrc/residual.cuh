@@ -7,6 +7,7 @@
 #pragma once
 
 #include <initializer_list>
+#include <mutex>
 
 #include "elements.cuh"
 #include "internal.h"
@@ -224,14 +225,31 @@ template <typename P> void set_rows(const avggt_rows* t, int size, P* data, int6
 }
 
 constexpr int kSmemPerSm = 224 * 1024, kSmemPerBlock = 2048;       // what blocks can have; a block's own, beside the pipeline
+constexpr int kMostSmem = kSmemPerSm - kSmemPerBlock;              // of a block's pipeline and sums
 
-template <typename... P>
-cudaError_t launch_with_smem(void (*kernel)(P...), int64_t blocks, unsigned threads, int smem, cudaStream_t st, const P&... args) {
+// Allows an instance the most that any call asks of it, once for each device.  (The limit belongs to the function: set to each call's own
+// size, it could be lowered by another host thread between a call's setting and its launch.)
+template <auto KERNEL> cudaError_t allow_smem() {
+  static std::mutex mu;
+  static bool ready[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  if (ready[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
+  ready[dev] = e == cudaSuccess;
+  return e;
+}
+
+template <auto KERNEL, typename A>
+cudaError_t launch_with_smem(int64_t blocks, unsigned threads, int smem, cudaStream_t st, const A& args) {
   if (smem > 40 * 1024) {            // with the kernels' own, below what needs no asking
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = allow_smem<KERNEL>();
     if (e != cudaSuccess) return e;
   }
-  return launch_dependent(kernel, static_cast<unsigned>(blocks), threads, smem, st, args...);
+  return launch_dependent(KERNEL, static_cast<unsigned>(blocks), threads, smem, st, args);
 }
 
 // Threads of a row: eight channels each, sixteen where that would be more than 512.

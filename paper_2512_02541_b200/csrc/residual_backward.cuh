@@ -454,9 +454,10 @@ cudaError_t launch_backward_rows(ResidualBackArgs a, unsigned threads, cudaStrea
   if (LAY > 2 && a.stages * stage + sums + kSmemPerBlock > kSmemPerSm)    // wide rows of many bytes: no room for a pipeline
     return launch_backward_rows<TR, TB, 2, true, 512, RUNS, R>(a, threads, st);
   const int64_t blocks = BLOCK ? a.segments : (a.segments + kWarpRows - 1) / kWarpRows;
-  const auto kernel = a.post == AVGGT_NORM_NONE ? residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>
-                                                : residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>;
-  return launch_with_smem(kernel, blocks, threads, a.stages * stage + sums, st, a);
+  const int smem = a.stages * stage + sums;
+  return a.post == AVGGT_NORM_NONE
+             ? launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>>(blocks, threads, smem, st, a)
+             : launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>>(blocks, threads, smem, st, a);
 }
 
 template <typename TR, typename TB, int LAY>

@@ -240,9 +240,9 @@ cudaError_t launch_forward_rows(ResidualArgs a, unsigned threads, int sm_count, 
   const int64_t batches = (static_cast<int64_t>(a.n_tokens) + R - 1) / R;
   int64_t blocks = BLOCK ? batches : (batches + kWarpRows - 1) / kWarpRows;
   if (blocks > static_cast<int64_t>(sm_count) * per_sm) blocks = static_cast<int64_t>(sm_count) * per_sm;
-  const auto kernel = a.post == AVGGT_NORM_NONE ? residual_norm_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>
-                                                : residual_norm_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>;
-  return launch_with_smem(kernel, blocks, threads, a.stages * stage, st, a);
+  return a.post == AVGGT_NORM_NONE
+             ? launch_with_smem<residual_norm_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>>(blocks, threads, a.stages * stage, st, a)
+             : launch_with_smem<residual_norm_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>>(blocks, threads, a.stages * stage, st, a);
 }
 
 template <typename TR, typename TB, int LAY>
