@@ -50,6 +50,22 @@ class Standard:
         return self.rstd * u_err + self.rstd * np.abs(u) * (self.rel + 2 * U)
 
 
+def residual_forward(op, x, y, weight=None, bias=None, gate=None, post_weight=None, post_bias=None):
+    """-> what r and h of ``op`` (block_oracle.Residual) may be off by in front of their rounding."""
+    n = x.shape[0]
+    rows = lambda t, fallback: np.abs(op.rows(t, n, fallback))
+    r = op.forward(x, y, weight, bias, gate, post_weight, post_bias)[0]
+    sy = Standard(y, op.post, op.post_eps)
+    g, pw, pb = rows(gate, 1.0), rows(post_weight, 1.0), rows(post_bias, 0.0)
+    r_err = g * (pw * sy.err + 5 * U * (pw * np.abs(sy.xhat) + pb)) + U * np.abs(op.scale * np.asarray(x, np.float64)) + U * np.abs(r)
+    if op.norm == orc.NONE:
+        return {"r": r_err}
+    st = Standard(r, op.norm, op.eps)
+    moved = st.rstd * (r_err + (mean(r_err) if op.norm == orc.LAYER else 0.0) + np.abs(st.xhat) * mean(r_err * np.abs(st.xhat)))
+    a = np.abs(op.factor(weight, n))
+    return {"r": r_err, "h": a * (st.err + moved) + 4 * U * (a * np.abs(st.xhat) + rows(bias, 0.0))}
+
+
 def residual_backward(op, dh, dr, r, y, weight=None, bias=None, gate=None, post_weight=None, post_bias=None):
     """-> of each gradient that ``op`` (block_oracle.Residual) gives: {name: what it may be off by in front of its rounding}."""
     n = (dr if dr is not None else r).shape[0]
@@ -111,11 +127,11 @@ def half_step(want, step, smallest):
 
 
 def beyond(got, want, bounds, residual=(0.0, 0.0), branch=(0.0, 0.0)):
-    """-> {name: largest error / bound} of the gradients whose error passes its bound somewhere, or is not a number.  got, want: {name:
-    array}; residual, branch: (eps, smallest value) of the types of dx and of dy."""
+    """-> {name: largest error / bound} of the results whose error passes its bound somewhere, or is not a number.  got, want: {name:
+    array}; residual, branch: (eps, smallest value) of the types of r and dx and of h and dy."""
     out = {}
     for name, bound in bounds.items():
-        step = residual if name == "dx" else branch if name == "dy" else (0.0, 2.0 ** -150)
+        step = residual if name in ("r", "dx") else branch if name in ("h", "dy") else (0.0, 2.0 ** -150)
         with np.errstate(over="ignore"):
             ratio = np.abs(got[name] - want[name]) / (bound + half_step(want[name], *step))
         if not (ratio <= 1).all():
