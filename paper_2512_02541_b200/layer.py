@@ -110,12 +110,14 @@ class SubsampledGlobalAttention:
         """The layer from the heads of a projection: ``rotary`` (an ``AxialRotary``) normalises and turns Q and K, and the layer, or with
         ``frame`` the frame attention of a converted block, follows on the same stream.
 
-        q, k, v: bf16 [N*L, H, d], strided as the (fused) projection leaves them; V is copied only where it is not contiguous.
+        q, k, v: bf16 [N*L, H, d], strided as the (fused) projection leaves them; V is copied only where it is not
+        contiguous, or not aligned to 16 bytes as the attention asks for.
         positions: int32 [N*L, axes] (``token_positions``).  Weights and biases of the heads' norms: float32 [d], or None.
         """
         if any(t.dtype is not torch.bfloat16 or t.shape != self._shape for t in (q, k, v)):
             raise ValueError(f"expected bf16 tensors of shape {tuple(self._shape)}")
-        Q, K, V = rotary.forward(q, k, positions, v=None if v.is_contiguous() else v, q_weight=q_weight, q_bias=q_bias, k_weight=k_weight,
+        as_it_is = v.is_contiguous() and v.data_ptr() % 16 == 0
+        Q, K, V = rotary.forward(q, k, positions, v=None if as_it_is else v, q_weight=q_weight, q_bias=q_bias, k_weight=k_weight,
                                  k_bias=k_bias)
         attend = self.frame_attend if frame else self.forward
         return attend(Q, K, v if V is None else V, out=out)
