@@ -340,8 +340,13 @@ int avggt_frame_attn(const avggt_params* p, const void* Q, const void* K, const 
  *   - zero tokens are allowed: nothing is read, outputs per token have no element, gradients of weights are zero;
  *   - an output may be the very array that an input is (same address, same strides) where that is said; otherwise outputs must not
  *     overlap inputs or one another.
- * A row that holds an infinity or a NaN gives NaN in its own outputs and in the sums over tokens, nowhere else.  Squares are summed
- * in 32 bits: values beyond 1e18 overflow their row's norm, as in any 32-bit norm.
+ * Values that are not finite stay in their row (of the rotary entry points: their head), and come out of it only by way of the sums
+ * over tokens.  Behind a layer norm, and where they are NaN behind either norm, all of the row's normalised values and gradients are
+ * NaN.  An infinity makes an RMS norm's deviation infinite: finite values of the row are 0 times the weight plus the bias, the infinite
+ * one is NaN; gradients through that norm are NaN in the whole row.  Without a norm they stay in their channel, or in their pair of
+ * elements: a pair that holds an infinity gives NaN beside it where its cosine or sine is 0 (position 0, pairs that are not turned).
+ * Squares are summed in 32 bits: a row whose squares (less the mean's) add up to more than 3.4e38, as 8,192 values of 2e17 do, has an
+ * infinite deviation like one that holds an infinity, as in any 32-bit norm.
  */
 #define AVGGT_TYPE_BF16 0
 #define AVGGT_TYPE_FP16 1
