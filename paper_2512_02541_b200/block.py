@@ -17,9 +17,9 @@ _TYPES = {torch.bfloat16: B.AVGGT_TYPE_BF16, torch.float16: B.AVGGT_TYPE_FP16, t
 _F32 = torch.float32
 _contiguous = torch.contiguous_format
 # what torch.cuda.current_device() and torch.cuda.current_stream(index).cuda_stream give, without what they do on the way (there is a
-# CUDA tensor in hand where these are called)
-_current_device = getattr(torch._C, "_cuda_getDevice", None)
-_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# CUDA tensor in hand where these are called); themselves where this torch does not have the short forms
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 RotaryGrads = namedtuple("RotaryGrads", "dq dk dv q_weight q_bias k_weight k_bias")
 ResidualGrads = namedtuple("ResidualGrads", "dx dy weight bias gate post_weight post_bias")
