@@ -7,6 +7,7 @@ checks in general form and ctypes structures, of which the kernel is 4).
 """
 
 import ctypes
+import operator
 from collections import namedtuple
 
 import torch
@@ -212,11 +213,17 @@ class ResidualNorm:
         r = residual_scale * x + gate * post_norm(y),     h = norm(r) * weight + bias
 
     ``norm`` and ``post_norm``: AVGGT_NORM_* in front of the next branch and behind the last one.  ``one_plus_weight``: 1 + weight
-    multiplies the norm.  A weight, bias or gate of shape [groups, channels] has a row for every ``tokens_per_group`` tokens.
+    multiplies the norm.  A weight, bias or gate of shape [groups, channels] has a row for every ``tokens_per_group`` tokens; weight
+    and bias, where both are given, have the same shape.
     """
 
     def __init__(self, channels, *, norm=B.AVGGT_NORM_LAYER, eps=1e-5, post_norm=B.AVGGT_NORM_NONE, post_eps=1e-5, residual_scale=1.0,
                  one_plus_weight=False, tokens_per_group=None):
+        if tokens_per_group is not None:
+            try:
+                tokens_per_group = operator.index(tokens_per_group)
+            except TypeError:
+                raise ValueError(f"tokens_per_group: expected a whole number, not {tokens_per_group!r}") from None
         self.channels, self.norm, self.eps, self.post_norm, self.post_eps = channels, norm, eps, post_norm, post_eps
         self.residual_scale, self.one_plus_weight, self.tokens_per_group = residual_scale, one_plus_weight, tokens_per_group
 
@@ -228,8 +235,8 @@ class ResidualNorm:
         like = weight if weight is not None else bias
         grouped_w, grouped_g = like is not None and like.dim() == 2, gate is not None and gate.dim() == 2
         if grouped_w or grouped_g:
-            if per_group is None:
-                raise ValueError("a weight, bias or gate for each group needs tokens_per_group")
+            if per_group is None or per_group < 1:
+                raise ValueError("a weight, bias or gate for each group needs tokens_per_group of at least 1")
             groups = (-(-T // per_group), C)
             if grouped_w:
                 flags |= B.AVGGT_RESIDUAL_WEIGHT_GROUPED
