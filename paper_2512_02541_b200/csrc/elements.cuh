@@ -26,7 +26,6 @@ __device__ __forceinline__ uint32_t bits_of_two(float a, float b, const __half*)
 template <typename T, int N>
 struct Run {
   static constexpr int kBytes = N * static_cast<int>(sizeof(T));
-  static constexpr int kAlign = kBytes >= 16 ? 16 : kBytes;   // the alignment that load and store ask for
   uint32_t w[kBytes >= 4 ? kBytes / 4 : 1];
 
   __device__ __forceinline__ void load(const void* p) {
@@ -57,27 +56,9 @@ struct Run {
       *static_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
     }
   }
-  // The same by asynchronous copies to shared memory (runs of at least four bytes), in pieces of up to 16 bytes that lie `apart` bytes
-  // from one another there.  By way of the first-level cache: lanes' runs may share its sectors.
-  static __device__ __forceinline__ void load_async(uint32_t dst, uint32_t apart, const void* p) {
-    if constexpr (kBytes >= 16) {
-#pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i) copy_async<16, true>(dst + i * apart, static_cast<const uint4*>(p) + i);
-    } else {
-      copy_async<kBytes, true>(dst, p);
-    }
-  }
-  __device__ __forceinline__ void take(const unsigned char* p, uint32_t apart) {   // from where load_async put it
-    if constexpr (kBytes >= 16) {
-#pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p + i * apart);
-        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
-      }
-    } else {
-      load(p);
-    }
-  }
+  // The same by an asynchronous copy to shared memory (runs of 4, 8 or 16 bytes), from where load reads it.  By way of the first-level
+  // cache: lanes' runs may share its sectors.
+  static __device__ __forceinline__ void load_async(uint32_t dst, const void* p) { copy_async<kBytes, true>(dst, p); }
   // Two groups of four neighbouring elements, 128 elements apart: neighbouring lanes' groups are neighbours.  Groups from element `end`
   // on are zero.
   __device__ __forceinline__ void load_quads(const void* p, int end) {

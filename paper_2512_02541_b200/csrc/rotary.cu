@@ -29,8 +29,8 @@ constexpr int kMaxTable = 256;      // pairs of the tokens that a warp works on 
 constexpr int kMaxTokens = 8;       // of them, so that their positions on three axes are a warp's
 constexpr int kMaxSegs = 4;         // blocks of pairs: up to three axes, and the elements that are not turned
 
-// Stages of the pipeline of copies, of which all but one are in flight: 48 KB of an SM's.
-__host__ __device__ constexpr int stages_of(int stage_bytes) { return stage_bytes == 0 ? 0 : stage_bytes <= 8192 ? 4 : 3; }
+// Stages of the pipeline of copies, of which all but one are in flight.
+__host__ __device__ constexpr int stages_of(int stage_bytes) { return stage_bytes == 0 ? 0 : 4; }
 
 struct RotaryTensor {
   const char* in;                   // forward: the heads; backward: the gradient of the turned heads
@@ -151,31 +151,29 @@ struct HeadRuns {
   using R = Run<T, PU>;
   using Units = LaneUnits<T, PU, NU, ADJ>;
   static constexpr bool kAsync = R::kBytes >= 4;
-  static constexpr int kPieces = R::kBytes > 16 ? R::kBytes / 16 : 1;
-  static constexpr int kPieceBytes = R::kBytes / kPieces;
-  static constexpr int kApart = 32 * kWarps * kPieceBytes;                 // bytes between a thread's pieces
-  static constexpr int kStageBytes = kAsync ? 2 * NU * kPieces * kApart : 0;
+  static constexpr int kApart = 32 * kWarps * R::kBytes;                   // bytes between a thread's runs
+  static constexpr int kStageBytes = kAsync ? 2 * NU * kApart : 0;
   R lo[NU], hi[NU];
 
-  static __device__ __forceinline__ void fetch(uint32_t own, const char* p, const Units& u) {   // own: the thread's first piece in the stage
+  static __device__ __forceinline__ void fetch(uint32_t own, const char* p, const Units& u) {   // own: the thread's first run in the stage
 #pragma unroll
     for (int i = 0; i < NU; ++i)
       if (u.have[i]) {
-        R::load_async(own + 2 * i * kPieces * kApart, kApart, p + u.lo[i]);
-        R::load_async(own + (2 * i + 1) * kPieces * kApart, kApart, p + u.hi[i]);
+        R::load_async(own + 2 * i * kApart, p + u.lo[i]);
+        R::load_async(own + (2 * i + 1) * kApart, p + u.hi[i]);
       }
   }
   static __device__ __forceinline__ void clear(unsigned char* own, int bytes) {
     if constexpr (kAsync)
       for (int at = 0; at < bytes; at += kApart)
 #pragma unroll
-        for (int w = 0; w < kPieceBytes; w += 4) *reinterpret_cast<uint32_t*>(own + at + w) = 0u;
+        for (int w = 0; w < R::kBytes; w += 4) *reinterpret_cast<uint32_t*>(own + at + w) = 0u;
   }
   __device__ __forceinline__ void take(const unsigned char* own) {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      lo[i].take(own + 2 * i * kPieces * kApart, kApart);
-      hi[i].take(own + (2 * i + 1) * kPieces * kApart, kApart);
+      lo[i].load(own + 2 * i * kApart);
+      hi[i].load(own + (2 * i + 1) * kApart);
     }
   }
   __device__ __forceinline__ void load(const char* p, const Units& u, bool on) {
@@ -392,7 +390,7 @@ __global__ void __launch_bounds__(32 * kWarps, kBlocksPerSm) rotary_kernel(const
   constexpr int kStageBytes = Runs::kStageBytes, kStages = stages_of(kStageBytes);
   const int lane = threadIdx.x & 31, lanes = LANES > 0 ? LANES : a.lanes;
   const RotarySmem s = rotary_smem<GROUPS>(smem + kStages * kStageBytes);
-  const uint32_t own = threadIdx.x * Runs::kPieceBytes;
+  const uint32_t own = threadIdx.x * Runs::R::kBytes;
   Runs::clear(smem + own, kStages * kStageBytes);
   const Share share(a, GROUPS);
   const RotaryTensor& t = a.t[share.which];
@@ -517,7 +515,7 @@ __global__ void __launch_bounds__(32 * kWarps, kBackBlocksPerSm) rotary_backward
   constexpr int kStageBytes = 2 * Runs::kStageBytes, kStages = stages_of(kStageBytes);     // a head's gradient and its input
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lanes = LANES > 0 ? LANES : a.lanes;
   const RotarySmem s = rotary_smem<GROUPS>(smem + kStages * kStageBytes);
-  const uint32_t own = threadIdx.x * Runs::kPieceBytes;
+  const uint32_t own = threadIdx.x * Runs::R::kBytes;
   Runs::clear(smem + own, kStages * kStageBytes);
   const Share share(a, GROUPS);
   const RotaryTensor& t = a.t[share.which];
@@ -734,6 +732,8 @@ struct RotaryVariant {
 template <typename T, int PU, int NU, bool ADJ, int LANES, bool BACK>
 RotaryVariant rotary_variant(bool groups) {
   constexpr int stage = (BACK ? 2 : 1) * HeadRuns<T, PU, NU, ADJ>::kStageBytes, smem = stages_of(stage) * stage;
+  // with the sums of the gradient, what a thread block has without asking
+  static_assert(smem + kWarps * 2 * kMaxTable * 4 + (BACK ? 2 * kWarps * 2 * kMaxPairs * 4 : 0) <= 48 * 1024, "shared memory");
   const int bytes = smem + kWarps * 2 * table_pairs(groups) * 4;
   if constexpr (BACK)
     return {groups ? rotary_backward_kernel<T, PU, NU, ADJ, LANES, true> : rotary_backward_kernel<T, PU, NU, ADJ, LANES, false>, bytes};
@@ -763,15 +763,6 @@ RotaryVariant rotary_instance_of(int type, bool adjacent, int pu, int lanes, boo
     case AVGGT_TYPE_FP16: return adjacent ? rotary_instance<__half, true, BACK>(pu, lanes, groups) : rotary_instance<__half, false, BACK>(pu, lanes, groups);
     default: return adjacent ? rotary_instance<float, true, BACK>(pu, lanes, groups) : rotary_instance<float, false, BACK>(pu, lanes, groups);
   }
-}
-
-cudaError_t launch_variant(const RotaryVariant& v, unsigned blocks, int smem, cudaStream_t st, const RotaryArgs& a) {
-  smem += v.smem;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-  }
-  return launch_dependent(v.kernel, blocks, 32 * kWarps, smem, st, a);
 }
 
 // Pairs, blocks of pairs, axes and frequencies.
@@ -915,7 +906,8 @@ cudaError_t launch_rotary(const avggt_rotary_params& p, int sm_count, const int3
   const int64_t chunks = a.t[0].chunks + a.t[1].chunks + a.t[2].chunks;
   a.split = a.n_tokens * chunks <= static_cast<int64_t>(sm_count) * kBlocksPerSm * kWarps ? 1 : 0;
   const unsigned blocks = share_blocks(&a, sm_count * kBlocksPerSm, 4, 3, 3);
-  return launch_variant(rotary_instance_of<false>(p.type, adjacent, pu, a.lanes, groups), blocks, 0, st, a);
+  const RotaryVariant v = rotary_instance_of<false>(p.type, adjacent, pu, a.lanes, groups);
+  return launch_dependent(v.kernel, blocks, 32 * kWarps, v.smem, st, a);
 }
 
 cudaError_t launch_rotary_backward(const avggt_rotary_params& p, int sm_count, const int32_t* positions, const avggt_heads* const in[3],
@@ -938,7 +930,8 @@ cudaError_t launch_rotary_backward(const avggt_rotary_params& p, int sm_count, c
   const int pu = choose_unit(a, type_size(p.type), adjacent);
   const bool groups = set_units(&a, pu);
   const unsigned blocks = share_blocks(&a, sm_count * kBackBlocksPerSm, 7, 3, 5);
-  const cudaError_t e = launch_variant(rotary_instance_of<true>(p.type, adjacent, pu, a.lanes, groups), blocks, 2 * kWarps * a.d * 4, st, a);
+  const RotaryVariant v = rotary_instance_of<true>(p.type, adjacent, pu, a.lanes, groups);
+  const cudaError_t e = launch_dependent(v.kernel, blocks, 32 * kWarps, v.smem + 2 * kWarps * a.d * 4, st, a);
   if (e != cudaSuccess) return e;
   RotarySums r = {};
   r.partials = a.partials;
