@@ -192,10 +192,9 @@ struct Staged {
         for (uint32_t b = 0; b < kPiece; b += 4) *reinterpret_cast<uint32_t*>(at + k * kApart + b) = 0u;
   }
 };
-__device__ __forceinline__ void wait_stages(int stages) {
+__device__ __forceinline__ void wait_stages(int stages) {      // two or three
   if (stages == 2) copy_async_wait<0>();
-  else if (stages == 3) copy_async_wait<1>();
-  else copy_async_wait<2>();
+  else copy_async_wait<1>();
 }
 
 // ---- launches

@@ -447,17 +447,21 @@ __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_
 
 template <typename TR, typename TB, int LAY, bool BLOCK, int THREADS, int RUNS, int R>
 cudaError_t launch_backward_rows(ResidualBackArgs a, unsigned threads, cudaStream_t st) {
-  const int stage = LAY > 2 ? THREADS * R * RUNS * 2 * kRun * static_cast<int>(sizeof(TR) + sizeof(TB)) : 0;
+  constexpr int stage = LAY > 2 ? THREADS * R * RUNS * 2 * kRun * static_cast<int>(sizeof(TR) + sizeof(TB)) : 0;
   const int sums = a.smem_sums ? static_cast<int>(threads) * 2 * RUNS * kRun * 4 : 0;
-  const int per_sm = kBackwardThreads / static_cast<int>(threads);
-  a.stages = per_sm * (3 * stage + sums + kSmemPerBlock) <= kSmemPerSm ? 3 : 2;
-  if (LAY > 2 && a.stages * stage + sums + kSmemPerBlock > kSmemPerSm)    // wide rows of many bytes: no room for a pipeline
+  if constexpr (2 * stage > kMostSmem) {                 // wide rows of 32 bits on both sides: no room for a pipeline
     return launch_backward_rows<TR, TB, 2, true, 512, RUNS, R>(a, threads, st);
-  const int64_t blocks = BLOCK ? a.segments : (a.segments + kWarpRows - 1) / kWarpRows;
-  const int smem = a.stages * stage + sums;
-  return a.post == AVGGT_NORM_NONE
-             ? launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>>(blocks, threads, smem, st, a)
-             : launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>>(blocks, threads, smem, st, a);
+  } else {
+    if (LAY > 2 && 2 * stage + sums > kMostSmem)         // nor for one with wide rows' sums behind it
+      return launch_backward_rows<TR, TB, 2, true, 512, RUNS, R>(a, threads, st);
+    const int per_sm = kBackwardThreads / static_cast<int>(threads);
+    a.stages = per_sm * (3 * stage + sums + kSmemPerBlock) <= kSmemPerSm ? 3 : 2;
+    const int64_t blocks = BLOCK ? a.segments : (a.segments + kWarpRows - 1) / kWarpRows;
+    const int smem = a.stages * stage + sums;
+    return a.post == AVGGT_NORM_NONE
+               ? launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, false>>(blocks, threads, smem, st, a)
+               : launch_with_smem<residual_backward_kernel<TR, TB, LAY, BLOCK, THREADS, RUNS, R, true>>(blocks, threads, smem, st, a);
+  }
 }
 
 template <typename TR, typename TB, int LAY>
