@@ -1,9 +1,10 @@
 """What stands around the attention of a block: rotary positions with the norm of the heads, and the residual stream with its norms
 and gate, forward and backward.  PyTorch is used for device memory and streams only: the calls enqueue the library's kernels on
-the current stream of the inputs' device and are not recorded by autograd; gradients are computed by the ``backward`` methods.
+the current stream of the inputs' device and are not recorded by autograd, whatever requires a gradient (results carry no graph);
+gradients are computed by the ``backward`` methods.
 
 The checks are written to be cheap: a call on few tokens is as long as the host takes for it (a frame's rotary positions: 24 us with
-checks in general form and ctypes structures, of which the kernel is 4).
+checks in general form and ctypes structures, 15 as they are, of which the kernel runs for 8).
 """
 
 import ctypes

@@ -46,9 +46,11 @@ cudaError_t residual_backward_wide(const ResidualBackArgs& a, int type, int layo
 namespace {
 
 // R rows go through together, as in the forward kernel; they are read again from their stage where they are needed, which leaves the
-// registers to the sums and parameters.  A batch ends where a group does.  30 frames of 1,024 channels in bf16 (507 MB): 80 us, 6.3 TB/s,
-// and 6 us for the sums over segments; with a post norm and the stream in 32 bits (2,048 channels, 619 MB) 115 us and 10: there the latency of
-// the exchanges among a row's eight warps, two blocks of them on an SM, bounds it.
+// registers to the sums and parameters.  A batch ends where a group does.  30 frames of 1,024 channels in bf16 (507 MB): 82 us, 6.2 TB/s,
+// and 6 us for the sums over segments; with a post norm and the stream in 32 bits (2,048 channels, 619 MB) 116 us and 10: there the latency of
+// the exchanges among a row's eight warps, two blocks of them on an SM, bounds it.  Of the 112 variants 42 spill registers: a warp's rows
+// behind a post norm (up to 236 bytes a thread stored), rows above 4,096 channels (48 to 180) and rows of single channels (24 to 92, above
+// 4,096 channels 428 to 944).  The two above do not.
 template <typename TR, typename TB, int LAY, bool BLOCK, int THREADS, int RUNS, int R, bool POST>
 __global__ void __launch_bounds__(THREADS, kBackwardThreads / THREADS) residual_backward_kernel(const __grid_constant__ ResidualBackArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];

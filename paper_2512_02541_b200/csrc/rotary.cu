@@ -505,9 +505,10 @@ __global__ void __launch_bounds__(32 * kWarps, kBlocksPerSm) rotary_kernel(const
 //                                                           first: rstd^3 leaves the range of 32 bits long before rstd does)
 //   dweight = sum of e * xhat, dbias = sum of e            over tokens and heads
 // The sums are kept by the lane that holds the elements, over all the tokens of its warp; a thread block works on one tensor, so that a
-// lane has one tensor's sums to keep.  The blocks' sums go to the workspace and are added up by rotary_sums_kernel.  With 64 registers of
-// sums and weights and twelve warps on the SM the issue of instructions (52% of the slots) and their latency bound it: 30 frames 101 us,
-// 5 TB/s; with four blocks on the SM the registers spill (151 us).
+// lane has one tensor's sums to keep.  The blocks' sums go to the workspace and are added up by rotary_sums_kernel.  With 48 registers of
+// sums and weights, 16 of cosines and sines and twelve warps on the SM the issue of instructions (50% of the slots) and their latency
+// bound it: 30 frames 102 us, 5 TB/s; with four blocks on the SM the registers spill (151 us).  As it is, of the 72 variants seven spill 4 to
+// 20 bytes a thread, six of them runs of eight where the number of lanes is not known to the compiler.
 template <typename T, int PU, int NU, bool ADJ, int LANES, bool GROUPS>
 __global__ void __launch_bounds__(32 * kWarps, kBackBlocksPerSm) rotary_backward_kernel(const __grid_constant__ RotaryArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
