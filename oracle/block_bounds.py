@@ -6,6 +6,8 @@ U = 2^-24 is the largest relative error of one operation.  Counted to first orde
                                  the terms themselves fewer than ROW = 70 errors of the sum of absolute terms
   a sum over tokens              rows of a segment, then a 32nd part of the segments, then five steps: CHAIN = 140 for up to 4000 tokens
                                  (thread blocks take at least one and, at that many tokens, at most 28 rows each)
+  a sum over a group's tokens    rows of a segment, then the group's segments one behind the other, which are no more together than the
+                                 group has tokens and one, and the factors behind them: its tokens and 8
 A result is rounded to its type once, by at most half a step of its value (`half_step`), or of the type's smallest value.
 """
 
@@ -71,7 +73,11 @@ def residual_backward(op, dh, dr, r, y, weight=None, bias=None, gate=None, post_
     n = (dr if dr is not None else r).shape[0]
     bounds = {}
     per_token = lambda t, fallback: np.abs(op.rows(t, n, fallback))
-    summed = lambda terms, errors, like: op.summed(errors, like) + CHAIN * U * op.summed(np.abs(terms), like)
+
+    def summed(terms, errors, like):
+        chain = CHAIN if like.ndim == 1 else min(op.per_group, n) + 8
+        return op.summed(errors, like) + chain * U * op.summed(np.abs(terms), like)
+
     d, d_err = (0.0, 0.0) if dr is None else (np.asarray(dr, np.float64), 0.0)
     if dh is not None:
         dh = np.asarray(dh, np.float64)

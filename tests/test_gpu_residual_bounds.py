@@ -67,3 +67,11 @@ def test_a_segments_rows_in_the_shared_memory_sums():
         pr = Problem(400, 8192, FP32, BF16, "rms", post, "group", grouped=True, per_group=1)
         assert pr.T > torch.cuda.get_device_properties(0).multi_processor_count * 2
         check(pr)
+
+
+@pytest.mark.parametrize("per_group", (1200, 2400, 5))
+def test_sums_of_one_row_that_every_token_repeats(per_group):
+    """Gradients of stride 0, where the roundings of a sum all go the same way."""
+    pr = Problem(2400, 264, FP32, FP32, post="rms", gate="group", grouped=True, per_group=per_group)
+    pr.dh, pr.dr = pr.dh[:1].expand(2400, 264), pr.dr[:1].expand(2400, 264)
+    check(pr)
